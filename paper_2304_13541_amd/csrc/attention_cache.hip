@@ -25,7 +25,6 @@ namespace {
 
 typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
-typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
 
 constexpr float LOG2E = 1.4426950408889634f;
 // Sums are rescaled once a score passes their reference by 2^SLACK, not at
@@ -282,22 +281,28 @@ struct Groups {
 template <int DH, int FORMAT, int SUBS>
 struct Step;
 
+// A lane's dims of its query row: eight for each product, product j those from
+// 32 j + 8 g on (STRIDE 8, STEP 32) or from DH / 4 g + 8 j on (STRIDE DH / 4, STEP
+// 8), as the keys' lanes have them.
+template <int DH, int STRIDE, int STEP>
+struct QueryRow {
+  bf16x8 q[DH / 32];
+  __device__ __forceinline__ void load(const bf16* p, bool aligned, bool live, int g) {
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) q[j] = query(p + STRIDE * g + STEP * j, aligned, live);
+  }
+  __device__ __forceinline__ void convert(float sign) {
+    if (sign == 1.f) return;
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) q[j] = with_sign(q[j], sign);
+  }
+};
+
 // bf16: K fragments straight from memory, a tile's 32 dims at a time.
 template <int DH, int SUBS>
 struct Step<DH, KV_BF16, SUBS> {
   static constexpr int WORDS = DH / 32;  // of a lane's dims of a value row
-  struct Query {
-    bf16x8 q[DH / 32];
-    __device__ __forceinline__ void load(const bf16* p, bool aligned, bool live, int g) {
-#pragma unroll
-      for (int j = 0; j < DH / 32; ++j) q[j] = query(p + 32 * j + 8 * g, aligned, live);
-    }
-    __device__ __forceinline__ void convert(float sign) {
-      if (sign == 1.f) return;
-#pragma unroll
-      for (int j = 0; j < DH / 32; ++j) q[j] = with_sign(q[j], sign);
-    }
-  };
+  typedef QueryRow<DH, 8, 32> Query;
   bf16x8 k[SUBS * 2][DH / 32];
   unsigned v[SUBS][8][WORDS];
   __device__ __forceinline__ void load_k(const Groups<SUBS>& gr, const KVView& kv, int head, int c, int g) {
@@ -338,79 +343,34 @@ struct Step<DH, KV_BF16, SUBS> {
   }
 };
 
-// 4 bits: keys go into the scaled product as they lie in the cache (lane: key
-// c, block g of 32 dims, its scale beside it).  Its other operand has 8 bits,
-// so a query row is two of them: x = 2^e (hi + lo), hi the nearest e4m3 value
-// (four significant bits), lo the exact rest, which fits in e4m3 again: bf16
-// has eight bits.  Exact for dims down to 2^-10 of the row's largest; below,
-// off by at most 2^-18 of it.  For 64 dims the two parts lie side by side in
-// one product of depth 128, against the keys twice.
+// 4 bits: a lane loads dims DH / 4 g .. of key c, eight to a word, and turns each
+// word to bf16 for its product.  (The scaled product takes 4-bit keys as they lie,
+// but its other operand has 8 bits: a query row in two e4m3 parts under one scale
+// is exact only for dims down to 2^-9 of its largest, and in three e5m2 parts down
+// to 2^-23; the rest of a small dim is lost.  48 sequences of one row, 128 units
+// of 32 rows and 64 of 35 take 103, 46 and 43.8 us with two parts, 117, 51 and 48.7
+// with three and 100.5, 46.7 and 44.8 by conversion.)
 template <int DH, int SUBS>
 struct Step<DH, KV_FP4, SUBS> {
   static constexpr int WORDS = DH / 32;
-  static constexpr int PARTS = DH / 64;
-  struct Query {
-    bf16x8 v[2 * PARTS];
-    i32x8 q[PARTS];
-    int scale;  // byte of 2^e (255: a value is not finite)
-    __device__ __forceinline__ void load(const bf16* p, bool aligned, bool live, int g) {
-#pragma unroll
-      for (int t = 0; t < 2 * PARTS; ++t)  // dims 16 g .. and, of 128, 64 + 16 g ..
-        v[t] = query(p + 64 * (t >> 1) + 16 * g + 8 * (t & 1), aligned, live);
-    }
-    __device__ __forceinline__ void convert(float sign) {
-      float x[16 * PARTS], top = 0.f, bad = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2 * PARTS; ++t) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[8 * t + e] = (float)v[t][e] * sign;
-          top = fmaxf(top, fabsf(x[8 * t + e]));
-          bad = fmaf(x[8 * t + e], 0.f, bad);
-        }
-      }
-      top = quad_max(bad != 0.f ? INFINITY : top);
-      const int ex = (int)(__float_as_uint(top) >> 23) - 127;  // 2^ex <= top
-      const int e = max(ex - 7, -126);
-      scale = ex == 128 ? 255 : e + 127;
-      const float inv = ex == 128 ? 0.f : __uint_as_float((unsigned)(127 - e) << 23);
-      unsigned hi[4 * PARTS], lo[4 * PARTS];
-#pragma unroll
-      for (int w = 0; w < 4 * PARTS; ++w) {
-        float y[4], r[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = x[4 * w + j] * inv;
-        int h = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-        h = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], h, true);
-        r[0] = y[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0);
-        r[1] = y[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1);
-        r[2] = y[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2);
-        r[3] = y[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3);
-        int l = __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false);
-        l = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], l, true);
-        hi[w] = (unsigned)h;
-        lo[w] = (unsigned)l;
-      }
-      // an 8-bit operand's lane g holds depths 16 g .. and 64 + 16 g ..
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        q[0][w] = (int)hi[w];
-        q[0][4 + w] = (int)(PARTS == 2 ? hi[4 * (PARTS - 1) + w] : lo[w]);
-        if constexpr (PARTS == 2) {
-          q[1][w] = (int)lo[w];
-          q[1][4 + w] = (int)lo[4 + w];
-        }
-      }
-    }
-  };
-  u32x4 k[SUBS * 2];
+  typedef QueryRow<DH, DH / 4, 8> Query;
+  unsigned k[SUBS * 2][DH / 32];
   unsigned ks[SUBS * 2];
   unsigned v[SUBS][8];
   unsigned vs[SUBS][2];  // scales of four keys each
   __device__ __forceinline__ void load_k(const Groups<SUBS>& gr, const KVView& kv, int head, int c, int g) {
-    const int block = DH == 128 ? g : g & 1;
-    const unsigned at = c * (DH / 2) + block * 16, sat = (block << kv.shift) + c;
-    gr.template each<DH / 2>(kv, kv.k, head, [&](int i, const char* p) { k[i] = *reinterpret_cast<const u32x4*>(p + at); });
+    const unsigned at = c * (DH / 2) + g * (DH / 8), sat = ((g * (DH / 4) / KV_BLOCK) << kv.shift) + c;
+    gr.template each<DH / 2>(kv, kv.k, head, [&](int i, const char* p) {
+      if constexpr (DH == 128) {
+        const u32x4 t = *reinterpret_cast<const u32x4*>(p + at);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) k[i][w] = t[w];
+      } else {
+        const u32x2 t = *reinterpret_cast<const u32x2*>(p + at);
+        k[i][0] = t[0];
+        k[i][1] = t[1];
+      }
+    });
     gr.template scales<DH>(kv, kv.ks, head, [&](int i, const unsigned char* p) { ks[i] = *(p + sat); });
   }
   __device__ __forceinline__ void load_v(const Groups<SUBS>& gr, const KVView& kv, int head, int c, int g) {
@@ -426,11 +386,11 @@ struct Step<DH, KV_FP4, SUBS> {
     });
   }
   __device__ __forceinline__ f32x4 scores(int i, const Query& q) const {
-    const i32x8 a = {(int)k[i][0], (int)k[i][1], (int)k[i][2], (int)k[i][3], 0, 0, 0, 0};
+    const float scale = kv_scale_of(ks[i]);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < PARTS; ++x)
-      s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.q[x], s, 4, 0, 0, (int)ks[i], 0, q.scale);
+    for (int j = 0; j < DH / 32; ++j)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv_fp4_values(k[i][j], scale), q.q[j], s, 0, 0, 0);
     return s;
   }
   __device__ __forceinline__ void values(int b, unsigned (&out)[8][WORDS]) const {
