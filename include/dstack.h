@@ -827,9 +827,12 @@ dstack_status dstack_op_attention(const void* qkv, int B, int T, int heads, int 
  *   sum_j softmax_j(scale * q_h . k_j) v_j over the visible keys j of its
  *   sequence on key head h / (heads / kv_heads): j <= p and, with window > 0,
  *   j > p - window or j < sinks (sinks first tokens stay visible).  No visible
- *   key (or scores of -infinity only): 0.  What is stored at a key that no row of the call's sequence sees,
- *   or that this row does not see, does not change its output, NaN and
- *   infinities included.  fp32 scores, softmax and sums; the weights are
+ *   key (or scores of -infinity only): 0.  What is stored at a key that no row
+ *   of the call's sequence sees, or that this row does not see, does not change
+ *   its output, NaN and infinities included; one in a value that the row sees
+ *   makes its dim of the output infinite or NaN, however small the key's weight
+ *   is.  Finite values whose magnitude times the row's keys is below 2^119 do
+ *   not overflow.  fp32 scores, softmax and sums; the weights are
  *   rounded to bf16 for the product with the values.  q bf16 (row r at q + r
  *   * q_stride elements, heads of dh; append's q_out or packed rows), out bf16
  *   [rows][heads][dh].  max_q: rows of the longest sequence (rows past it are

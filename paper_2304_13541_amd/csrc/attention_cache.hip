@@ -116,10 +116,24 @@ __device__ __forceinline__ float poison(unsigned w, float acc) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), z, acc, false);
 }
 
-// Infinities and NaN among values that some rows of a tile see and others do
-// not: 0 * infinity would reach the rows that do not.  They are taken out of
-// the values and noted in LDS for the rows that see them, two bits a dim (+inf
-// 1, -inf 2, NaN 3), to be added to the rows' sums at the end.
+template <int WORDS>
+__device__ __forceinline__ bool not_finite(const unsigned (&val)[8][WORDS]) {
+  float bad = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) bad = poison(val[j][w], bad);
+  return bad != 0.f;
+}
+
+// Infinities and NaN among values: 0 * infinity is NaN in a row that does not
+// see the key, in one whose weight of it is below what fp32 holds, and in sums
+// rescaled past it.  They are taken out of the values and noted in LDS for the
+// rows that see them, two bits a dim (+inf 1, -inf 2, NaN 3), to be added to the
+// rows' sums at the end.  The few-row kernel looks for them on the way (bf16: one
+// operation for two values, which costs nothing beside the reads; 4 bits: the
+// scales alone, 2 to 3% where vector work bounds it); the tile kernel, whose
+// values go through LDS, takes a unit again, looking, where a sum ended as NaN.
 __device__ __forceinline__ unsigned odd_bits(unsigned x) {  // of a bf16 value
   const unsigned a = x & 0x7fffu;
   return a > 0x7f80u ? 3u : a < 0x7f80u ? 0u : x >> 15 ? 2u : 1u;
@@ -159,6 +173,16 @@ __device__ __forceinline__ bf16x8 with_sign(bf16x8 v, float sign) {
   return v;
 }
 
+// a row's output from its sums (0: no visible key)
+__device__ __forceinline__ f32x4 normed(f32x4 v, float sum) {
+  return sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * (1.f / sum);
+}
+
+// The factor of a part whose maximum is m beside the whole's M: at least fp32's
+// least value, so that a part's infinities stay what they are (0 * infinity is
+// NaN).  It adds at most 2^-149 of the part's sums to the whole's.
+__device__ __forceinline__ float part_factor(float m, float M) { return fmaxf(exp2_fast(m - known(M)), 0x1p-149f); }
+
 __device__ __forceinline__ void store_out(bf16* p, f32x4 v, bool aligned) {
   const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
   if (aligned) {
@@ -194,7 +218,6 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, __amdgpu_buffer_
     const int rr = x / (DH / 4), d = x % (DH / 4) * 4;
     float mm = -INFINITY;
     for (int sp = 0; sp < parts; ++sp) mm = fmaxf(mm, lds[sp * rows + rr]);
-    const float M = known(mm);
     float sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < parts; s0 += 8) {
@@ -206,13 +229,12 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, __amdgpu_buffer_
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         if (s0 + k < parts) {
-          const float f = exp2_fast(lds[(s0 + k) * rows + rr] - M);
+          const float f = part_factor(lds[(s0 + k) * rows + rr], mm);
           sum += lds[MERGE_ROWS + (s0 + k) * rows + rr] * f;
           o += v[k] * f;
         }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    store_out(dst(rr) + d, o * inv, o16);
+    store_out(dst(rr) + d, normed(o, sum), o16);
   }
 }
 
@@ -341,6 +363,8 @@ struct Step<DH, KV_BF16, SUBS> {
 #pragma unroll
       for (int w = 0; w < WORDS; ++w) out[j][w] = v[b][j][w];
   }
+  // whether all values are known to be finite
+  __device__ __forceinline__ bool finite() const { return false; }
 };
 
 // 4 bits: a lane loads dims DH / 4 g .. of key c, eight to a word, and turns each
@@ -405,6 +429,15 @@ struct Step<DH, KV_FP4, SUBS> {
         out[j][3] = kv_fp4_pair<3>(v[b][j], s);
       }
     }
+  }
+  // by the scales: of less than 252, 2^125, no value is past bf16's range
+  __device__ __forceinline__ bool finite() const {
+    unsigned large = 0;  // the top bits of bytes of 252 and more
+#pragma unroll
+    for (int b = 0; b < SUBS; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) large |= ((vs[b][h] & 0x7f7f7f7fu) + 0x04040404u) & vs[b][h];
+    return !__any(large & 0x80808080u);
   }
 };
 
@@ -667,7 +700,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
     if (more) begin();
     if (!first) {
       const int rows = done.toks * a.group;
-      const bool several = done.toks > 1;
       const bool single = done_ta == 0 && done_tb == done.count;
       auto result = [&](int rr, int d) {
         const int tok = a.by_group.div(rr);
@@ -676,7 +708,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
       // where workgroup b keeps its piece: the one it starts in (0) or the one it ends in (1)
       const unsigned mine = (2 * blockIdx.x + (done_ta == 0 ? 1 : 0)) * slot_bytes;
       const int ml_at = a.part_rows * DH * 4;
-      if (several) __syncthreads();  // every wave is done with lds as the place of odd values
       const float sum_l = quad_sum(l);
       if (g == 0) {
         ms[wave][c] = m;
@@ -709,12 +740,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
             sum += ls[s0 + w][row] * f;
             o += *reinterpret_cast<const f32x4*>(lds + ((s0 + w) * 16 + row) * PITCH + d) * f;
           }
-          if (several && noted) {
+          if (noted) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += odd_of<DH>(notes, rr, d + e);
           }
           if (single) {
-            store_out(result(rr, d), o * (sum == 0.f ? 0.f : 1.f / sum), o16);
+            store_out(result(rr, d), normed(o, sum), o16);
           } else {
             __builtin_amdgcn_raw_buffer_store_b128(o, room, (int)(mine + (rr * DH + d) * 4), 0, CPOL_SC1);
             if (d == 0) {
@@ -771,14 +802,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) nm = fmaxf(nm, __int_as_float(ml[k][0]));
-                const float f = exp2_fast(pm - known(nm));
+                const float f = part_factor(pm, nm);
                 pm = nm;
                 pl *= f;
                 po *= f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                   if (b + k * groups > b1) continue;
-                  const float h = exp2_fast(__int_as_float(ml[k][0]) - known(nm));
+                  const float h = part_factor(__int_as_float(ml[k][0]), nm);
                   pl += __int_as_float(ml[k][1]) * h;
                   po += v[k] * h;
                 }
@@ -794,14 +825,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
               if (group == 0) {
                 for (int k = 1; k < groups; ++k) {
                   const float* from = lds + (k * shares + y) * 8;
-                  const float nm = fmaxf(pm, from[4]), f = exp2_fast(pm - known(nm)), h = exp2_fast(from[4] - known(nm));
+                  const float nm = fmaxf(pm, from[4]), f = part_factor(pm, nm), h = part_factor(from[4], nm);
                   pm = nm;
                   pl = pl * f + from[5] * h;
                   po = po * f + *reinterpret_cast<const f32x4*>(from) * h;
                 }
               }
             }
-            if (y < shares && group == 0) store_out(result(rr, d), po * (pl == 0.f ? 0.f : 1.f / pl), o16);
+            if (y < shares && group == 0) store_out(result(rr, d), normed(po, pl), o16);
           }
           __syncthreads();
         }
@@ -811,12 +842,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
     first = false;
     const Range rg = un.rg;
     const int rows = un.toks * a.group;
-    const bool several = un.toks > 1;
-    if (several) {
-      if (threadIdx.x == 0) noted = 0;
-      for (int y = threadIdx.x; y < FEW_ROWS * (DH / 16); y += THREADS) notes[y] = 0u;
-      __syncthreads();
-    }
+    if (threadIdx.x == 0) noted = 0;
+    for (int y = threadIdx.x; y < rows * (DH / 16); y += THREADS) notes[y] = 0u;
+    __syncthreads();
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
@@ -869,31 +897,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
         const u32x4 w = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
         p[b] = __builtin_bit_cast(bf16x8, w);
       }
+      const bool plain = whole && st.finite();
 #pragma unroll
       for (int b = 0; b < SUBS; ++b) {
         unsigned val[8][S::WORDS];
         st.values(b, val);
-        if (!whole) {
-          // a value that no row sees counts nothing, whatever it is
-          float bad = 0.f;
+        if (!plain) {
+          if (!whole) {
+            // a value that no row sees counts nothing, whatever it is
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int key = key0 + 32 * b + (j >> 2) * 16 + 4 * g + (j & 3);
-            const bool seen = (have >> (2 * b + (j >> 2)) & 1) && key < rg.end && (key >= rg.lo_first || key < rg.sinks);
+            for (int j = 0; j < 8; ++j) {
+              const int key = key0 + 32 * b + (j >> 2) * 16 + 4 * g + (j & 3);
+              const bool seen = (have >> (2 * b + (j >> 2)) & 1) && key < rg.end && (key >= rg.lo_first || key < rg.sinks);
 #pragma unroll
-            for (int w = 0; w < S::WORDS; ++w) {
-              val[j][w] = seen ? val[j][w] : 0u;
+              for (int w = 0; w < S::WORDS; ++w) val[j][w] = seen ? val[j][w] : 0u;
             }
           }
-          if (several) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-              for (int w = 0; w < S::WORDS; ++w) bad = poison(val[j][w], bad);
-          }
-          if (__any(bad != 0.f)) {
+          if (__any(not_finite(val))) {
             if (lane == 0) noted = 1;
-            unsigned* mine = reinterpret_cast<unsigned*>(lds) + (wave * 64 + lane) * (8 * S::WORDS);
+            static_assert(64 * 8 * S::WORDS <= 16 * PITCH, "a wave's values fit where it leaves its sums");
+            unsigned* mine = reinterpret_cast<unsigned*>(lds) + wave * (16 * PITCH) + lane * (8 * S::WORDS);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -1098,13 +1121,8 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(KVView kv, AttendAr
   }
 
   f32x16 acc[DH / 32];
-#pragma unroll
-  for (int i = 0; i < DH / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
-  float m = -INFINITY, l = 0.f;
-
-  bool noted = false;
+  float m, l;
+  bool careful = false;  // the second time: a sum was NaN
   for (int x = threadIdx.x; x < TILE_ROWS * (DH / 16); x += 256) notes[x] = 0u;
 
   Loader<DH, FORMAT> ld;
@@ -1119,151 +1137,153 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(KVView kv, AttendAr
     if (lane == 0) there[t & 1][wave] = page >= 0;
     ld.start(kv, page, kvh, key & ((1 << kv.shift) - 1), lds0 + ((t - t0) & 1 ? 2 * TILE_BYTES : 0), wave);
   };
-  if (t0 < t_end) {
-    look(t0);
-    load(t0);
-    look(t0 + 1);
-  }
-  for (int t = t0; t < t_end; ++t) {
-    const int key0 = tiles[t] * TILE_KEYS;
-    const unsigned buf = (t - t0) & 1 ? 2 * TILE_BYTES : 0;
-    ld.finish(lds + buf);
-    __syncthreads();  // the tile is in LDS; every wave is done with the one before, whose place the next one takes
-    const int have = __builtin_amdgcn_readfirstlane(there[t & 1][0] | there[t & 1][1] << 1 | there[t & 1][2] << 2 | there[t & 1][3] << 3);
-    if (t + 1 < t_end) {
-      load(t + 1);
-      look(t + 2);
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    if (t0 < t_end) {
+      look(t0);
+      load(t0);
+      look(t0 + 1);
     }
-    unsigned char* K = lds + buf;
-    unsigned char* V = K + TILE_BYTES;
-    // values of 16 keys x: lanes of one half take keys 4 h + j and 8 + 4 h + j, dim 32 i + c
-    auto value = [&](int i, int x) {
-      u32x4 r;
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int key = 16 * x + 8 * y + 4 * h + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        const unsigned char* at = V + key * (DH * 2) + v_piece<DH>(key, piece) * 16 + (lane & 1) * 8;
-        const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(const __attribute__((address_space(3))) void*)at);
-        const u32x2 d = __builtin_bit_cast(u32x2, w);
-        r[2 * y] = d[0];
-        r[2 * y + 1] = d[1];
+    for (int t = t0; t < t_end; ++t) {
+      const int key0 = tiles[t] * TILE_KEYS;
+      const unsigned buf = (t - t0) & 1 ? 2 * TILE_BYTES : 0;
+      ld.finish(lds + buf);
+      __syncthreads();  // the tile is in LDS; every wave is done with the one before, whose place the next one takes
+      const int have = __builtin_amdgcn_readfirstlane(there[t & 1][0] | there[t & 1][1] << 1 | there[t & 1][2] << 2 | there[t & 1][3] << 3);
+      if (t + 1 < t_end) {
+        load(t + 1);
+        look(t + 2);
       }
-      return r;
-    };
-    if (have != 15 || key0 + TILE_KEYS - 1 > rg.p0 || key0 + TILE_KEYS > rg.end ||
-        (key0 < rg.lo_last && key0 + TILE_KEYS > rg.sinks)) {
-      // Some rows do not see all of it.  Values that none sees become zero,
-      // whatever they are; infinities and NaN that some see are counted by
-      // themselves and taken out.
-      bool odd = false;
-      constexpr int PER = DH / 4 / 8;  // 16-byte pieces of a thread: a quarter of a key
-      const int key = threadIdx.x >> 2, j = key0 + key;
-      const bool seen = (have >> (key >> 4) & 1) && j < rg.end && (j >= rg.lo_first || j < rg.sinks);
-      u32x4* mine = reinterpret_cast<u32x4*>(V + key * (DH * 2)) + (threadIdx.x & 3) * PER;
+      unsigned char* K = lds + buf;
+      unsigned char* V = K + TILE_BYTES;
+      // values of 16 keys x: lanes of one half take keys 4 h + j and 8 + 4 h + j, dim 32 i + c
+      auto value = [&](int i, int x) {
+        u32x4 r;
 #pragma unroll
-      for (int x = 0; x < PER; ++x) {
-        if (!seen) {
-          mine[x] = u32x4{0u, 0u, 0u, 0u};
-        } else {
-          const u32x4 w = mine[x];
-          float bad = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bad = poison(w[e], bad);
-          odd = odd || bad != 0.f;
+        for (int y = 0; y < 2; ++y) {
+          const int key = 16 * x + 8 * y + 4 * h + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+          const unsigned char* at = V + key * (DH * 2) + v_piece<DH>(key, piece) * 16 + (lane & 1) * 8;
+          const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(const __attribute__((address_space(3))) void*)at);
+          const u32x2 d = __builtin_bit_cast(u32x2, w);
+          r[2 * y] = d[0];
+          r[2 * y + 1] = d[1];
         }
-      }
-      if (__syncthreads_or(odd)) {
-        noted = true;
-#pragma unroll 1
-        for (int x = 0; x < PER; ++x) {
-          u32x4 w = mine[x];
-          const int dim = 8 * v_piece<DH>(key, (threadIdx.x & 3) * PER + x);
+        return r;
+      };
+      if (careful || have != 15 || key0 + TILE_KEYS - 1 > rg.p0 || key0 + TILE_KEYS > rg.end ||
+          (key0 < rg.lo_last && key0 + TILE_KEYS > rg.sinks)) {
+        // Some rows do not see all of it: values that none sees become zero, whatever they are.
+        constexpr int PER = DH / 4 / 8;  // 16-byte pieces of a thread: a quarter of a key
+        const int key = threadIdx.x >> 2, j = key0 + key;
+        const bool seen = (have >> (key >> 4) & 1) && j < rg.end && (j >= rg.lo_first || j < rg.sinks);
+        u32x4* mine = reinterpret_cast<u32x4*>(V + key * (DH * 2)) + (threadIdx.x & 3) * PER;
+        if (!seen) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            note_odd<DH>(notes, w[e], dim + 2 * e, rows, [&](int r) {
-              const int pr = rg.p0 + token(r);
-              return j <= pr && (j >= window_start(pr, a.window) || j < rg.sinks);
-            });
-            w[e] = without_odd(w[e]);
+          for (int x = 0; x < PER; ++x) mine[x] = u32x4{0u, 0u, 0u, 0u};
+        } else if (careful) {
+#pragma unroll 1
+          for (int x = 0; x < PER; ++x) {
+            u32x4 w = mine[x];
+            const int dim = 8 * v_piece<DH>(key, (threadIdx.x & 3) * PER + x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              note_odd<DH>(notes, w[e], dim + 2 * e, rows, [&](int r) {
+                const int pr = rg.p0 + token(r);
+                return j <= pr && (j >= window_start(pr, a.window) || j < rg.sinks);
+              });
+              w[e] = without_odd(w[e]);
+            }
+            mine[x] = w;
           }
-          mine[x] = w;
         }
         __syncthreads();
       }
-    }
-    if (key0 <= pos_last && (key0 + TILE_KEYS > low_first || key0 < rg.sinks)) {
-      f32x16 s[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
-#pragma unroll
-      for (int j = 0; j < DH / 16; ++j)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {  // two sums in turn: neither waits for its last product
-          const int key = 32 * b + c;
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(K + key * (DH * 2) + k_piece<DH>(key, 2 * j + h) * 16);
-          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[j], s[b], 0, 0, 0);
-        }
-      // eight reads ahead of the products (as the compiler orders them: 2-4% slower)
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-      for (int j = 0; j < DH / 8; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      const bool whole = have == 15 && key0 + TILE_KEYS - 1 <= pos_first && key0 + TILE_KEYS <= rg.end &&
-                         (key0 >= low_last || key0 + TILE_KEYS <= rg.sinks);
-      if (!whole) {
+      if (key0 <= pos_last && (key0 + TILE_KEYS > low_first || key0 < rg.sinks)) {
+        f32x16 s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = key0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3);
-            const bool seen = (have >> (2 * b + (r >> 3)) & 1) && j < rg.end && j <= pos && (j >= low || j < rg.sinks);
-            s[b][r] = seen ? s[b][r] : -INFINITY;
+          for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < DH / 16; ++j)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {  // two sums in turn: neither waits for its last product
+            const int key = 32 * b + c;
+            const bf16x8 kf = *reinterpret_cast<const bf16x8*>(K + key * (DH * 2) + k_piece<DH>(key, 2 * j + h) * 16);
+            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[j], s[b], 0, 0, 0);
           }
-      }
-      float mx = s[0][0];
+        // eight reads ahead of the products (as the compiler orders them: 2-4% slower)
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-      mx = half_max(mx) * cs;
-      if (__any(mx > m + SLACK)) {
-        const float nm = fmaxf(m, mx), f = exp2_fast(m - known(nm));
-        m = nm;
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < DH / 32; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][r] *= f;
-      }
-      const float ref = known(m);
-      bf16x8 p[4];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float e[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            e[r] = exp2_fast(s[b][8 * x + r] * cs - ref);
-            l += e[r];
-          }
-          const u32x4 w = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
-          p[2 * b + x] = __builtin_bit_cast(bf16x8, w);
+        for (int j = 0; j < DH / 8; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        const bool whole = have == 15 && key0 + TILE_KEYS - 1 <= pos_first && key0 + TILE_KEYS <= rg.end &&
+                           (key0 >= low_last || key0 + TILE_KEYS <= rg.sinks);
+        if (!whole) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < DH / 32; ++i)
-          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value(i, x)), p[x], acc[i], 0, 0, 0);
+            for (int r = 0; r < 16; ++r) {
+              const int j = key0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3);
+              const bool seen = (have >> (2 * b + (r >> 3)) & 1) && j < rg.end && j <= pos && (j >= low || j < rg.sinks);
+              s[b][r] = seen ? s[b][r] : -INFINITY;
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+        mx = half_max(mx) * cs;
+        if (__any(mx > m + SLACK)) {
+          const float nm = fmaxf(m, mx), f = exp2_fast(m - known(nm));
+          m = nm;
+          l *= f;
+#pragma unroll
+          for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][r] *= f;
+        }
+        const float ref = known(m);
+        bf16x8 p[4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float e[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              e[r] = exp2_fast(s[b][8 * x + r] * cs - ref);
+              l += e[r];
+            }
+            const u32x4 w = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+            p[2 * b + x] = __builtin_bit_cast(bf16x8, w);
+          }
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int i = 0; i < DH / 32; ++i)
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value(i, x)), p[x], acc[i], 0, 0, 0);
+      }
     }
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) nan |= acc[i][r] != acc[i][r];
+    if (careful || !__syncthreads_or(nan)) break;
+    careful = true;
   }
 
-  if (noted) {
+  if (careful) {
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i)
 #pragma unroll
@@ -1272,7 +1292,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(KVView kv, AttendAr
   l += __shfl_xor(l, 32, 64);
   const bool valid = wave * 32 + c < rows;
   if (parts == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = 1.f / l;
     bf16* dst = a.out + (row_at * a.heads + head) * DH;
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i)
@@ -1284,7 +1304,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(KVView kv, AttendAr
         for (int y = 0; y < 2; ++y)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            w[y][e] = pack_bf16x2(acc[i][8 * x + 4 * y + 2 * e] * inv, acc[i][8 * x + 4 * y + 2 * e + 1] * inv);
+            w[y][e] = l == 0.f ? 0u : pack_bf16x2(acc[i][8 * x + 4 * y + 2 * e] * inv, acc[i][8 * x + 4 * y + 2 * e + 1] * inv);
         u32x4 o;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
