@@ -755,6 +755,13 @@ def attention(qkv, heads, out, stream=None):
 
 
 
+def _int32(what, bits):
+    """Refuses integers that the C call would take modulo 2^32; bits: their bitwise or (what is negative, the call
+    refuses itself)."""
+    if bits >> 31 not in (0, -1):
+        raise ValueError("%s must be below 2^31" % what)
+
+
 class KVCache:
     """Descriptor of a paged key/value cache (see dstack_kv_cache); keeps its tensors.
 
@@ -792,6 +799,7 @@ class KVBatch:
 
     def __init__(self, q_start, kv_len, page_table, rows):
         n, per = page_table.shape
+        _int32("KVBatch: sequences, pages and rows", n | per | int(rows))
         for t, count in ((q_start, n + 1), (kv_len, n), (page_table, n * per)):
             if t.numel() != count or not t.is_contiguous() or str(t.dtype) != "torch.int32":
                 raise ValueError("KVBatch: contiguous int32 q_start [n + 1], kv_len [n], page_table [n, pages]")
@@ -854,6 +862,7 @@ def kv_append(cache, batch, qkv, heads, cos_sin, q_out, pairs=False, stream=None
     n = rot = cs = 0
     if cos_sin is not None:
         n, rot = cos_sin.shape
+        n = min(n, 0x7fffffff)  # no position is past it
         cs = cos_sin.data_ptr()
         if cos_sin.dtype is not _fp32 or not cos_sin.is_contiguous() or cos_sin.get_device() != dev:
             raise ValueError("kv_append: cos_sin must be contiguous float32 on the cache's GPU")
@@ -871,6 +880,7 @@ def kv_read(cache, batch, k_out, v_out, stream=None):
 
 
 def attention_cache_workspace_bytes(rows, n_seq, heads, kv_heads, dh, max_q, max_kv, window=0, sinks=0):
+    _int32("attention_cache_workspace_bytes: sizes", rows | n_seq | heads | kv_heads | dh | max_q | max_kv | window | sinks)
     return lib().dstack_attention_cache_workspace_bytes(rows, n_seq, heads, kv_heads, dh, max_q, max_kv, window, sinks)
 
 
@@ -879,6 +889,7 @@ def attention_cache(q, cache, batch, out, max_q, max_kv, window=0, sinks=0, scal
     sqrt(dh); workspace: a device buffer whose first 16 KiB are zero before its first use, or None (see
     dstack_op_attention_cache)."""
     heads, rows, dh, dev = q.shape[1], batch.rows, cache.dh, cache.device
+    _int32("attention_cache: max_q, max_kv, window and sinks", max_q | max_kv | window | sinks)
     st = _cache_stream(cache, batch, stream, "attention_cache")
     p, stride = _rows_of(q, rows, heads * dh, "attention_cache: q", dev)
     ws, wsb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)

@@ -198,3 +198,20 @@ def test_workspace_bytes_of_bad_sizes():
     assert ds.attention_cache_workspace_bytes(0, 1, 1, 1, 64, 1, 10) == 0
     assert ds.attention_cache_workspace_bytes(1, 1, 3, 2, 64, 1, 10) == 0
     assert ds.attention_cache_workspace_bytes(1, 1, -1, 1, 64, 1, 10) == 0
+
+
+def test_integers_past_32_bits():
+    """A window of 2^32 + 5 is no window of 5: refused, not taken modulo 2^32."""
+    import torch
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype)  # noqa: E731
+    tensors = [z(*s, dtype=torch.int32) for s in ((2,), (1,), (1, 3))]
+    with pytest.raises(ValueError, match="below 2.31"):
+        ds.KVBatch(*tensors, (1 << 32) + 4)
+    c, b = ds.KVCache(z(2, 1, 16, 64), z(2, 1, 16, 64)), ds.KVBatch(*tensors, 4)
+    for kw in (dict(max_q=(1 << 32) + 1), dict(max_kv=1 << 31), dict(window=(1 << 32) + 5), dict(sinks=1 << 40),
+               dict(window=-(1 << 32) + 5)):
+        with pytest.raises(ValueError, match="below 2.31"):
+            ds.attention_cache(z(4, 1, 64), c, b, z(4, 1, 64), **{**dict(max_q=2, max_kv=32), **kw})
+        sizes = dict(rows=4, n_seq=1, heads=1, kv_heads=1, dh=64, max_q=2, max_kv=32)
+        with pytest.raises(ValueError, match="below 2.31"):
+            ds.attention_cache_workspace_bytes(**{**sizes, **kw})
