@@ -11,6 +11,12 @@
 // shares of the keys alike; many rows, tiles of keys in LDS that 128 rows
 // share.  Both keep the scores transposed (K Q^T), which leaves the weights
 // where the second product takes its operand from: no weight goes through LDS.
+// The weights are rounded to bf16 for that product, each by at most 2^-8 of it:
+// outputs of the timed cases are off by 0.0023 of their size, where rounding them
+// alone is 0.0017.  With what is left of each weight in a second product they are
+// off by 0.0017, but prompts take 375 us for 300, chunks on 4-bit keys 778 for 575
+// and 64 rows 159 for 133; single tokens 0 to 3% more, and are rounded alike so
+// that a row is as exact as a token as it is in a chunk.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -451,10 +457,10 @@ __device__ __forceinline__ u32x4 frag(const unsigned (&val)[8][WORDS], int i) {
   return t;
 }
 
-// Measured: 64 sequences, windows of 4096 of 32768 keys (8 heads of 128, bf16)
-// 193 us, 5.6 TB/s; 48 sequences of up to 16384 4-bit keys 97 us, 4.6 TB/s; one
-// of 131071 4-bit keys 36 us, 4.0 TB/s; one with 12 heads of 64, 64 keys, 8 us
-// after the append before it (the launch, the lookups and one join).
+// Measured: 64 sequences of 6000 to 32000 keys, windows of 4096 (8 heads of 128,
+// bf16) 192 us, 5.6 TB/s; 48 sequences of 1000 to 16000 4-bit keys 96 us, 4.6 TB/s;
+// one of 131071 4-bit keys 36 us, 4.0 TB/s; one with 12 heads of 64 and a window of
+// 128 keys 8 us (the launch, the lookups and one join).
 //
 // One unit = the rows of a sequence on one key head, FEW_ROWS at most.  The
 // call's units, each so many key tiles long, lie one behind the other; the
@@ -465,11 +471,10 @@ __device__ __forceinline__ u32x4 frag(const unsigned (&val)[8][WORDS], int i) {
 // sums; they are joined in LDS, and units that several workgroups hold a piece
 // of in memory, by the last of them to arrive.  (Waves of 32 rows, which read a
 // key half as often but whose sums leave no registers for loads ahead of the
-// join: 8 units of 32 rows on up to 8000 bf16 keys 39.5 us for 33.5, 64 units of
-// 35 rows on 4-bit keys 47.6 for 44.0.)
-// Tiles of a stretch at least: one a wave.  Of 2: 12 units of up to 65 keys 12.7
-// us for 10.5, 16 of 64 rows 41 for 36; of 32: 64 units of 35 rows on up to 7001
-// 4-bit keys 66 us for 43.
+// join: 32 units of 32 rows on up to 8000 bf16 keys 39.5 us for 33.5.)
+// Tiles of a stretch at least: one a wave.  Of 2: 12 units of 132 keys 12.9 us for
+// 10.6, 16 of 64 rows on 4-bit keys 40 for 36; of 32: 64 units of 35 rows on up to
+// 7001 4-bit keys 67 us for 46.
 constexpr int FEW_MIN_TILES = 8;
 constexpr int FEW_ROWS = 64;
 
@@ -568,7 +573,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
       const unsigned b = blockIdx.x;
       if (pieces && 2 * busy <= blocks && kv.n_seq <= 64) {
         // Few units: each is cut into equal parts of at most `chunk` tiles, one a workgroup, which then has one
-        // piece and ends after it (128 units of 32 rows 45 us, by stretches 51; 64 units of one row 19, 25).
+        // piece and ends after it (128 units of 32 rows 49 us, by stretches 51; 64 units of one token 19, 25).
         for (int k = 0; k < 2; ++k) {
           chunk = (int)(k ? quotient(whole_tiles, blocks - busy) : each) + 1;
           if (k == 0 && rest == 0) --chunk;
@@ -1063,9 +1068,9 @@ struct Loader<DH, KV_FP4> {
 // KB from LDS for 32 products of 32x32x16; 64 rows a wave would halve the reads,
 // but their sums and scores spill, and two groups of waves half a tile apart
 // took 355 us where this takes 308.  Bound by the vector work between the
-// products.  Measured: one prompt of 8192 rows, windows of 4096, 32 heads of
-// 128 on 8: 268 to 285 us, up to 900 TFLOP/s of the pairs that are visible; 2 x
-// 1024 rows on up to 16384 4-bit keys 509 to 546 us, up to 975 TFLOP/s.
+// products.  Measured: one prompt of 8192 rows, windows of 2048, 32 heads of 128
+// on 8: 284 us, 850 TFLOP/s of the pairs that are visible; 2 x 1024 rows on up to
+// 16000 4-bit keys 546 us, 910 TFLOP/s.
 template <int DH, int FORMAT>
 __global__ __launch_bounds__(256, 2) void attend_tile_kernel(KVView kv, AttendArgs a) {
   constexpr int TILE_BYTES = TILE_KEYS * DH * 2;
@@ -1367,19 +1372,19 @@ static AttendPlan attend_plan(int rows, int n_seq, int heads, int kv_heads, int 
   const long group = heads / kv_heads, most = std::min(max_q, rows) * group;
   const size_t room = ws_bytes > COUNTERS * 4 ? ws_bytes - COUNTERS * 4 : 0;
   // Up to 32 rows a unit the few-row kernel: 128 units of 32 rows on up to 8000
-  // 4-bit keys 45 us (by tiles 104), 32 units on bf16 keys 33 (38).  Up to 64
+  // 4-bit keys 48 us (by tiles 106), 32 units on bf16 keys 33 (41).  Up to 64
   // rows on 4-bit keys, which the tiles turn to bf16 for every wave alike: 48
-  // rows 68 (124), 35 rows 43 (57); four groups of rows read bf16 keys four
-  // times, 256 units of 64 rows 189 us (131).
+  // rows 74 (127), 35 rows 46 (60); four groups of rows read bf16 keys four
+  // times, 256 units of 64 rows 190 us (133).
   p.few = most <= (format == KV_FP4 ? FEW_ROWS : 32);
   if (p.few) {
     p.units = (long)n_seq * kv_heads;
     p.part_rows = (int)most;
     const size_t slots = 2 * (size_t)p.part_rows * (dh + 2) * 4;  // of a workgroup
     // Eight waves a workgroup join more of a unit in LDS and fewer pieces in
-    // memory: 8 units of 131071 4-bit keys 34 us (four waves: 37), 64 units of 35
-    // rows 43 (52).  Four leave less over between many units: 384 units 102 us
-    // (eight: 117), 192 units 25 (32).
+    // memory: 8 units of 131071 4-bit keys 34 us (four waves: 38), 64 units of 35
+    // rows 46 (53).  Four leave less over between many units: 384 units 100 us
+    // (eight: 113), 192 units 27 (32).
     p.waves = p.units <= n_cu / 4 ? 8 : 4;
     const long most_blocks = (long)n_cu * 8 / p.waves;  // two waves a SIMD
     const long whole = std::min(most_blocks, p.units), pieces = std::min<size_t>(room / slots, most_blocks);
@@ -1403,7 +1408,7 @@ static AttendPlan attend_plan(int rows, int n_seq, int heads, int kv_heads, int 
     // Parts for one workgroup a CU where each keeps 8 tiles, for two where it
     // keeps 16: four chunks of 64 rows on 8192 4-bit keys 131 -> 94 us by the
     // second, 256 rows on 32768 keys 255 -> 187; but units of 19 tiles cut in
-    // two 45 -> 53.
+    // two 43 -> 53.
     splits = std::max(std::min(n_cu / p.units, tiles / 8), std::min(2 * n_cu / p.units, tiles / 16));
     splits = std::min(splits, (long)(MERGE_ROWS / p.part_rows));
     splits = std::max(1L, std::min(splits, (long)std::min<size_t>(room / one, MERGE_ROWS)));
