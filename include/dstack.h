@@ -832,7 +832,8 @@ dstack_status dstack_op_attention(const void* qkv, int B, int T, int heads, int 
  *   its output, NaN and infinities included; one in a value that the row sees
  *   makes its dim of the output infinite or NaN, however small the key's weight
  *   is.  Finite values whose magnitude times the row's keys is below 2^119 do
- *   not overflow.  fp32 scores, softmax and sums; the weights are
+ *   not overflow.  scale: 0 or of magnitude 2^-126 to 2^126.  fp32 scores,
+ *   softmax and sums; the weights are
  *   rounded to bf16 for the product with the values.  q bf16 (row r at q + r
  *   * q_stride elements, heads of dh; append's q_out or packed rows), out bf16
  *   [rows][heads][dh].  max_q: rows of the longest sequence (rows past it are

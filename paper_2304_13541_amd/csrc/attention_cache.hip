@@ -535,7 +535,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_few_kernel(KVView kv, At
   const kv_uniform_ints starts = kv_uniform(kv.q_start), lens = kv_uniform(kv.kv_len);
   const bool pieces = a.part != nullptr;  // else whole units are dealt out
   const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f;
-  const float cs = a.scale == 0.f ? 1.f : fminf(fmaxf(fabsf(a.scale) * LOG2E, 1e-37f), 3e38f);
+  const float cs = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
   const bool q16 = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 15) == 0, o16 = ((uintptr_t)a.out & 15) == 0;
 
   // This workgroup's stretch [x, x_end) of the whole, and the sequence it
@@ -1107,7 +1107,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(KVView kv, AttendAr
   if (split >= parts) return;
   const int t0 = split * a.chunk, t_end = split == parts - 1 ? tiles.count : t0 + a.chunk;
   const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f;
-  const float cs = a.scale == 0.f ? 1.f : fminf(fmaxf(fabsf(a.scale) * LOG2E, 1e-37f), 3e38f);
+  const float cs = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
   const bool q16 = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 15) == 0, o16 = ((uintptr_t)a.out & 15) == 0;
 
   // the lane's row (past the end: the last one again), and those of the wave's first and last row
@@ -1458,7 +1458,8 @@ dstack_status launch_attention_cache(const dstack_kv_cache* c, const dstack_kv_b
   DS_CHECK(q_stride >= (int64_t)heads * c->dh, DSTACK_E_INVALID, "attention_cache: rows shorter than their heads");
   DS_CHECK(max_q >= 1 && max_kv >= 0 && window >= 0 && sinks >= 0, DSTACK_E_INVALID,
            "attention_cache: max_q >= 1, max_kv, window and sinks >= 0");
-  DS_CHECK(std::isfinite(scale), DSTACK_E_INVALID, "attention_cache: scale must be finite");
+  DS_CHECK(scale == 0.f || (std::fabs(scale) >= 0x1p-126f && std::fabs(scale) <= 0x1p126f), DSTACK_E_INVALID,
+           "attention_cache: scale must be 0 or of magnitude 2^-126 to 2^126");
   DS_CHECK(((uintptr_t)q & 1) == 0 && ((uintptr_t)out & 1) == 0, DSTACK_E_INVALID,
            "attention_cache: misaligned pointer");
   DS_CHECK(((uintptr_t)ws & 255) == 0, DSTACK_E_INVALID, "attention_cache: workspace must be 256-byte aligned");

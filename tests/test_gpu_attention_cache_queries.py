@@ -102,3 +102,17 @@ def test_rows_that_are_not_finite(env, n, fp4):
         ref = reference(b, cache, qb, heads, dh)
         check(b, got, ref, None)
     assert np.isnan(got[r, [1, 4, 6]]).all() and np.isfinite(np.delete(got[r], [1, 4, 6], 0)).all()
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("power", [-113, 113])
+def test_scale_near_its_ends(env, power, fp4):
+    """Scales of 2^-122 and 2^109 (of a range of 2^-126 to 2^126), the rows' size making up for them."""
+    heads, kvh, dh = 4, 1, 64
+    for n in (1, 40):
+        rng = np.random.default_rng(75)
+        b = kv_ref.Batch(rng, [n], [150], 16)
+        cache = filled(rng, b, kvh, dh, fp4)
+        qb = kv_ref.to_bf16_bits(np.ldexp(rng.standard_normal((b.rows, heads * dh)), power))
+        scale = 2.0 ** -power * 2.0 ** -(9 if power > 0 else 4)
+        check(b, attend(env, b, cache, qb, heads, kvh, dh, scale=scale), reference(b, cache, qb, heads, dh, scale), None)

@@ -215,3 +215,9 @@ def test_integers_past_32_bits():
         sizes = dict(rows=4, n_seq=1, heads=1, kv_heads=1, dh=64, max_q=2, max_kv=32)
         with pytest.raises(ValueError, match="below 2.31"):
             ds.attention_cache_workspace_bytes(**{**sizes, **kw})
+
+
+def test_scale_out_of_range():
+    """Scales whose product with log2 e fp32 does not hold are refused (they were taken as 1e-37 and 3e38)."""
+    for scale in (2.0 ** -127, -1e-40, 1e-45, 2.0 ** 126 * 1.01, -3e38):
+        assert attend(cache(), batch(), scale=scale) == ds.E_INVALID, scale
